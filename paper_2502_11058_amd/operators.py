@@ -3,7 +3,8 @@ cross entropy of a language model's head, each in the library's own kernels.
 
 Two forms of each.  `*_forward` and `*_backward` are the calls themselves: they check their tensors, allocate outputs and workspace
 with torch, and enqueue kernels on torch's current stream.  `norm`, `rotary`, `attention` and `linear_cross_entropy` are the same
-with gradients by autograd, for a model whose parameters `overlap.BackwardOverlap` holds.
+with gradients by autograd, for a model whose parameters `overlap.BackwardOverlap` holds.  Autograd does not record the kernels of a backward
+pass: a second derivative through any of them (`create_graph=True`) raises RuntimeError.
 
 Tensors are fp32 or bf16 (all of a call's tensors the same, statistics and losses fp32) on one GPU, which must be the current device.
 Their last dimension is contiguous; the others may have any strides.  Arguments that do not fit raise ValueError or TypeError, what the library
@@ -14,6 +15,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -345,6 +347,7 @@ class _Norm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, rstd, *mean = ctx.saved_tensors
         dx, dw, db = norm_backward(dy, x, weight, mean[0] if mean else None, rstd, kind=ctx.kind, bias=ctx.bias)
@@ -359,6 +362,7 @@ class _Rotary(torch.autograd.Function):
         return rotary_forward(q, k, table, positions, layout=layout)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         table, *positions = ctx.saved_tensors
         dq, dk = rotary_backward(dq, dk, table, positions[0] if positions else None, layout=ctx.layout)
@@ -374,6 +378,7 @@ class _Attention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         q, k, v, o, lse, *cu = ctx.saved_tensors
         cu_q, cu_k = cu if cu else (None, None)
@@ -388,6 +393,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         x, weight, targets, lse = ctx.saved_tensors
         dx, dw = linear_cross_entropy_backward(dloss, x, weight, targets, lse, need_dx=ctx.needs_input_grad[0], need_dweight=ctx.needs_input_grad[1])
