@@ -26,6 +26,7 @@ _SCALINGS = {"plain": B.DDP_ROTARY_PLAIN, "linear": B.DDP_ROTARY_LINEAR, "stretc
 
 
 _F32 = torch.float32
+_device = torch._C._cuda_getDevice  # the current one; asked only where a tensor is on a GPU
 
 
 # A small model's call is as long as its host side: a call looks at its tensors in a few expressions, and only what does not fit is
@@ -43,6 +44,9 @@ def _typed(first: torch.Tensor) -> int:
         raise TypeError(f"tensors have to be float32 or bfloat16, not {first.dtype}")
     if not first.is_cuda:
         raise ValueError("tensors have to be on a GPU")
+    # (the kernels go to the current device's stream: elsewhere they would run unordered with what makes and frees the tensors)
+    if first.get_device() != _device():
+        raise ValueError(f"tensors are on {first.device}, which is not the current device, cuda:{_device()}")
     return dtype
 
 
@@ -148,7 +152,7 @@ def rotary_table(rows: int, rotated: int, *, base: float = 10000.0, scaling: str
         raise ValueError(f"scaling has to be one of {sorted(_SCALINGS)}, not {scaling!r}")
     freq = B.ddp_rotary_frequencies(_SCALINGS[scaling], rotated, base, factor, low, high, context)
     table = torch.empty((rows, rotated // 2, 2), dtype=torch.float32, device=device or torch.device("cuda", torch.cuda.current_device()))
-    _need(table.is_cuda, "tensors have to be on a GPU")
+    _typed(table)
     B.ddp_rotary_table(rotated, freq, amplitude, rows, table)
     return table
 
