@@ -142,13 +142,20 @@ class Pretraining:
         rep.fill_peers_from(rep.flat, r, rep.ctx.ddp_slot_numel(slot))
 
     def iteration(self, r: int, tokens: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
+        """Behind what the current stream holds (tokens, peers' buffers), on the worker's own stream; what comes on the current stream
+        afterwards is behind it.  -> the loss, for the current stream."""
         ov = self.overlap
+        caller = torch.cuda.current_stream(self.rep.dev)
+        ov.main_stream.wait_stream(caller)
         with torch.cuda.stream(ov.main_stream):
             ov.begin(r, with_stats=False)
             loss = self.model.loss(self.params, tokens, targets, self.table)
             ov.backward(loss)
             ov.end()
-        return loss.detach()
+        caller.wait_stream(ov.main_stream)
+        loss = loss.detach()
+        loss.record_stream(caller)
+        return loss
 
     def close(self) -> None:
         self.overlap.close()
