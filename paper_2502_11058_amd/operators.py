@@ -199,6 +199,9 @@ def _rotary(q, k, table, positions, layout, inverse):
     if positions is not None:
         if positions.numel() != tokens:
             raise ValueError(f"{positions.numel()} positions for {tokens} tokens")
+        # (as many in another order, such as [tokens, batch], would turn tokens by each other's angles)
+        if positions.dim() != 1 and positions.shape != lead[:-2] and [n for n in positions.shape if n != 1] != [n for n in lead[:-2] if n != 1]:
+            raise ValueError(f"positions have to be {list(lead[:-2])} as the tokens are, or in one row, not {list(positions.shape)}")
         if positions.dtype not in (torch.int32, torch.int64):
             raise TypeError(f"positions have to be int32 or int64, not {positions.dtype}")
         if positions.device != q.device:
@@ -213,7 +216,7 @@ def _rotary(q, k, table, positions, layout, inverse):
 
 def rotary_forward(q: torch.Tensor, k: Optional[torch.Tensor], table: torch.Tensor, positions: Optional[torch.Tensor] = None, *, layout: str = "half"):
     """q [.., tokens, heads, dim] and k (or None) with the first 2 * pairs channels of each head rotated by their tokens' rows of the
-    table: `positions`, or the tokens' places in their sequence.  -> rotated q, rotated k."""
+    table: `positions` (int32 or int64 [.., tokens], or all in one row), or the tokens' places in their sequence.  -> rotated q, rotated k."""
     return _rotary(q, k, table, positions, layout, 0)
 
 
