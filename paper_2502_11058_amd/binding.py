@@ -422,8 +422,9 @@ def ddp_attention_forward(attention: ddp_attention, q: ddp_heads, k: ddp_heads, 
         return
     if rc is not None:
         _check(rc)
-    _check(lib().ddp_attention_forward(C.byref(attention), C.byref(q), C.byref(k), C.byref(v), _at(cu_q), _at(cu_k), C.byref(o), _at(lse), _at(workspace),
-                                       workspace_bytes, _stream_handle(stream)))
+    h = _heads_at
+    _check(lib().ddp_attention_forward(C.byref(attention), h(q), h(k), h(v), _at(cu_q), _at(cu_k), h(o), _at(lse), _at(workspace), workspace_bytes,
+                                       _stream_handle(stream)))
 
 
 def ddp_attention_backward_workspace(attention: ddp_attention, d_o: Optional[ddp_heads] = None, q: Optional[ddp_heads] = None, k: Optional[ddp_heads] = None,
@@ -441,8 +442,8 @@ def ddp_attention_backward(attention: ddp_attention, d_o: ddp_heads, q: ddp_head
         return
     if rc is not None:
         _check(rc)
-    r = C.byref
-    _check(lib().ddp_attention_backward(r(attention), r(d_o), r(q), r(k), r(v), r(o), _at(lse), _at(cu_q), _at(cu_k), r(dq), r(dk), r(dv), _at(workspace),
+    h = _heads_at
+    _check(lib().ddp_attention_backward(C.byref(attention), h(d_o), h(q), h(k), h(v), h(o), _at(lse), _at(cu_q), _at(cu_k), h(dq), h(dk), h(dv), _at(workspace),
                                         workspace_bytes, _stream_handle(stream)))
 
 
