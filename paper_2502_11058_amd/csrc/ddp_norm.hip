@@ -301,9 +301,11 @@ __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *part_w, co
 
 // Workgroups of the backward pass, each with a partial row: as many as keep enough bytes under way, and no more, since partial rows are written
 // and read again.  8192 x 768 fp32: 19.3 us with 512, 16.5 with 1024, 17.4 with 2048; 16384 x 4096 bf16: 79 us with 512, 86 with 768, 95 with 1024.
+// Rows that are not held have 64 runs of rows a column.
 int norm_parts(const ddp_norm &n) {
-    const int64_t groups = cdiv(n.cols * (int64_t)element_size(n.dtype), 16), most = groups <= 256 ? 1024 : 512;
-    return (int)(n.rows < most ? n.rows : most);
+    const int64_t groups = cdiv(n.cols * (int64_t)element_size(n.dtype), 16), most = groups <= 256 ? 1024 : groups <= 1024 ? 512 : 64;
+    const int64_t wgs = groups <= 256 ? cdiv(n.rows, 4) : n.rows;
+    return (int)(wgs < most ? wgs : most);
 }
 
 int check_norm(const char *who, const ddp_norm *n) {
@@ -419,18 +421,15 @@ extern "C" int ddp_norm_backward(const ddp_norm *norm, const void *dy, const voi
         a.part_b = dbias ? reinterpret_cast<float *>(static_cast<char *>(workspace) + part) : nullptr;
         return by_type(n, [&](auto t, auto rms) -> int {
             typedef decltype(t) T;
-            int used = 0;
             if (n.rows > 0)
                 by_length<T>(n.cols, [&](auto group, auto nv) {
                     if constexpr (nv.value > 0) {
-                        const int64_t wgs = cdiv(n.rows, 256 / group.value);
-                        used = (int)(wgs < parts ? wgs : parts);
                         by_size(n, 3, [&](auto past) {
-                            hipLaunchKernelGGL((norm_backward_kernel<T, rms.value, group.value, nv.value, past.value>), dim3((unsigned)used), dim3(256), 0, st, a);
+                            hipLaunchKernelGGL((norm_backward_kernel<T, rms.value, group.value, nv.value, past.value>), dim3((unsigned)parts), dim3(256), 0, st, a);
                         });
                     } else {
-                        used = parts < 64 ? parts : 64;  // (before dx, which may take the place of dy)
-                        if (columns) hipLaunchKernelGGL((norm_columns_kernel<T, rms.value>), dim3((unsigned)cdiv(n.cols, 256), (unsigned)used), dim3(256), 0, st, a);
+                        // (before dx, which may take the place of dy)
+                        if (columns) hipLaunchKernelGGL((norm_columns_kernel<T, rms.value>), dim3((unsigned)cdiv(n.cols, 256), (unsigned)parts), dim3(256), 0, st, a);
                         if (dx)
                             by_size(n, 3, [&](auto past) {
                                 hipLaunchKernelGGL((norm_backward_long_kernel<T, rms.value, past.value>), dim3((unsigned)(n.rows < 65536 ? n.rows : 65536)), dim3(256), 0, st, a);
@@ -438,7 +437,7 @@ extern "C" int ddp_norm_backward(const ddp_norm *norm, const void *dy, const voi
                     }
                 });
             if (columns)
-                hipLaunchKernelGGL((norm_fold_kernel<T>), dim3((unsigned)cdiv(n.cols, 32), dbias ? 2 : 1), dim3(1024), 0, st, a.part_w, a.part_b, used, n.cols,
+                hipLaunchKernelGGL((norm_fold_kernel<T>), dim3((unsigned)cdiv(n.cols, 32), dbias ? 2 : 1), dim3(1024), 0, st, a.part_w, a.part_b, parts, n.cols,
                                    static_cast<T *>(dweight), static_cast<T *>(dbias));
             return launched(who);
         });
