@@ -28,16 +28,18 @@ extern "C" {
  *                             RMS    mean = 0, otherwise the same;       y = h * weight (+ bias)
  * Backward, with g = dy * weight:  dx = rstd * (g - sum(g) / cols [LAYER] - h * sum(g * h) / cols)
  *                                  dweight = sum over rows of dy * h,  dbias = sum over rows of dy
- *   x, y, dy, dx       [rows, cols] of dtype; x_stride between the rows of x and dx, y_stride between those of y and dy
+ *   x, y, dy, dx       [rows, cols] of dtype; x_stride between the rows of x, y_stride between those of y and dy, dx_stride between those of
+ *                      dx (0: x_stride)
  *   weight, bias, dweight, dbias  [cols] of dtype; bias nullable
  *   mean, rstd         fp32 [rows], written by the forward call and read by the backward call; mean nullable for RMS
- *   dx nullable; dweight and dbias nullable (no workspace is needed without both).  dx may be dy if the strides agree. */
+ *   dx nullable; dweight and dbias nullable (no workspace is needed without both).  dx may be dy if their strides agree. */
 enum { DDP_NORM_LAYER = 0, DDP_NORM_RMS = 1 };
 typedef struct {
     int32_t kind, dtype;
     int64_t rows, cols;
     int64_t x_stride, y_stride;
     float eps;
+    int64_t dx_stride;
 } ddp_norm;
 int ddp_norm_forward(const ddp_norm *norm, const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd, void *stream);
 int64_t ddp_norm_backward_workspace(const ddp_norm *norm);

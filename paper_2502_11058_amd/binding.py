@@ -52,7 +52,7 @@ class ddp_opt(C.Structure):
 
 class ddp_norm(C.Structure):
     _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("x_stride", C.c_int64),
-                ("y_stride", C.c_int64), ("eps", C.c_float)]
+                ("y_stride", C.c_int64), ("eps", C.c_float), ("dx_stride", C.c_int64)]
 
 
 class ddp_rotary_shape(C.Structure):

@@ -123,6 +123,7 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(const NormArgs a) {
 struct NormBackArgs {
     NormArgs n;
     void *dx;
+    int64_t dx_stride;
     float *part_w, *part_b;  // [workgroups][cols], nullable
 };
 
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(const NormBackArgs a
         if (!a.dx) continue;
         s = group_sum2<GROUP>(s, scratch);
         const float c1 = RMS ? 0.0f : s.x * a.n.inv, c2 = s.y * a.n.inv;
-        T *dx = static_cast<T *>(a.dx) + row * a.n.x_stride;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (lane + k * GROUP) * N;
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(256) void norm_backward_long_kernel(const NormBackA
     const T *w = static_cast<const T *>(a.n.w);
     for (int64_t row = blockIdx.x; row < a.n.rows; row += gridDim.x) {
         const T *x = static_cast<const T *>(a.n.x) + row * a.n.x_stride, *dy = static_cast<const T *>(a.n.dy) + row * a.n.y_stride;
-        T *dx = static_cast<T *>(a.dx) + row * a.n.x_stride;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
         const float mean = RMS ? 0.0f : a.n.mean[row], rstd = a.n.rstd[row];
         f32x2 s{0.0f, 0.0f};
         for (int g = threadIdx.x; g < groups; g += 256) {
@@ -404,7 +405,9 @@ extern "C" int ddp_norm_backward(const ddp_norm *norm, const void *dy, const voi
         for (const void *p : {dy, x, weight, (const void *)dx, (const void *)dweight, (const void *)dbias})
             if (misaligned(p, e)) return bad(who, DDP_EALIGN, "a tensor is not aligned to its element type");
         if (misaligned(mean, 4) || misaligned(rstd, 4)) return bad(who, DDP_EALIGN, "mean or rstd is not aligned to its element type");
-        if (dx == dy && dx && n.x_stride != n.y_stride) return bad(who, DDP_EINVAL, "in place, the strides of dx and dy have to be the same");
+        const int64_t dx_stride = n.dx_stride ? n.dx_stride : n.x_stride;
+        if (dx && n.rows > 1 && (dx_stride < n.cols || reach(n.rows, dx_stride) < 0)) return bad(who, DDP_EINVAL, "dx_stride is smaller than cols or too large");
+        if (dx == dy && dx && n.rows > 1 && dx_stride != n.y_stride) return bad(who, DDP_EINVAL, "in place, the strides of dx and dy have to be the same");
         const int parts = norm_parts(n);
         const int64_t part = up((int64_t)parts * n.cols * 4, 256);
         if (columns && n.rows > 0) {
@@ -416,7 +419,7 @@ extern "C" int ddp_norm_backward(const ddp_norm *norm, const void *dy, const voi
         const hipStream_t st = static_cast<hipStream_t>(stream);
         NormBackArgs a{};
         a.n = norm_args(n);
-        a.n.x = x, a.n.dy = dy, a.n.w = weight, a.n.mean = const_cast<float *>(mean), a.n.rstd = const_cast<float *>(rstd), a.dx = dx;
+        a.n.x = x, a.n.dy = dy, a.n.w = weight, a.n.mean = const_cast<float *>(mean), a.n.rstd = const_cast<float *>(rstd), a.dx = dx, a.dx_stride = dx_stride;
         a.part_w = dweight ? static_cast<float *>(workspace) : nullptr;
         a.part_b = dbias ? reinterpret_cast<float *>(static_cast<char *>(workspace) + part) : nullptr;
         return by_type(n, [&](auto t, auto rms) -> int {

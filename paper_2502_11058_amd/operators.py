@@ -130,14 +130,13 @@ def norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean:
     if kind == "layer":
         _need(mean is not None, "mean is missing")
         _plain("mean", mean, (rows,), _F32, x)
-    # dx has x's strides
-    dx = torch.empty_like(xr) if stride == cols or rows <= 1 else torch.empty_strided(xr.shape, xr.stride(), dtype=x.dtype, device=x.device)
+    dx = _alike(x, xr)
     dw = torch.empty_like(weight)
     db = torch.empty_like(weight) if bias else None
-    shape = B.ddp_norm(_KINDS[kind], dtype, rows, cols, stride, dy_stride, 0.0)
+    shape = B.ddp_norm(_KINDS[kind], dtype, rows, cols, stride, dy_stride, 0.0, cols)
     n = B.ddp_norm_backward_workspace(shape)
     B.ddp_norm_backward(shape, dyr, xr, weight, mean, rstd, dx, dw, db, _workspace(n, x), n)
-    return dx if dx.shape == x.shape else dx.reshape(x.shape), dw, db
+    return dx, dw, db
 
 
 # ------------------------------------------------------------------------------------------------------------
