@@ -240,6 +240,8 @@ inline bool typed(int dtype) { return dtype == DDP_F32 || dtype == DDP_BF16; }
 inline bool misaligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 inline int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// The most workgroups of a launch: a dimension of a grid has less than 2^32 threads.  Of one that has more a part runs, without an error.
+constexpr int64_t most_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
 // Whether a call that moves so many bytes writes its results with streaming stores.  From the 256 MB of the last-level cache on they take less:
 // rotary positions of 16384 tokens, 40 heads of 128, 66 against 61 us, norm of 16384 x 4096 in bf16 forward 48 against 43, backward 83
 // against 77.  Below, what they save is lost by the next reader of the results: norm of 2048 x 4096 1.7 us less, a copy of its result 1.4 more.

@@ -91,12 +91,12 @@ struct Frequencies {
     double f[DDP_ROTARY_MAX_ROTATED / 2];
 };
 __global__ __launch_bounds__(256) void table_kernel(const Frequencies f, double amplitude, int64_t n, int half, float *table) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    double s, c;
-    sincos((double)(i / half) * f.f[i % half], &s, &c);
-    table[2 * i] = (float)(amplitude * c);
-    table[2 * i + 1] = (float)(amplitude * s);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        double s, c;
+        sincos((double)(i / half) * f.f[i % half], &s, &c);
+        table[2 * i] = (float)(amplitude * c);
+        table[2 * i + 1] = (float)(amplitude * s);
+    }
 }
 
 int check_side(const char *who, const void *x, const void *y, const ddp_rotary_shape &r, int heads, int64_t xt, int64_t xh, int64_t yt, int64_t yh) {
@@ -120,7 +120,7 @@ int launch_rotary(const ddp_rotary_shape &r, RotaryArgs &a, hipStream_t stream) 
     for (const int wide : {128, 256})
         if (up(per_token, wide) <= up(per_token, x)) x = wide;
     a.tokens_each = 256 / x;
-    while (cdiv(a.tokens, a.tokens_each) > 0x7fffffff) a.tokens_each *= 2;
+    while (cdiv(a.tokens, a.tokens_each) > most_groups(256)) a.tokens_each *= 2;
     const dim3 grid((unsigned)cdiv(a.tokens, a.tokens_each)), block((unsigned)x, (unsigned)(256 / x));
     const bool past = streams_past(2 * r.tokens * (r.q_heads + r.k_heads) * r.head_dim * (int64_t)sizeof(T));
     auto go = [&](auto interleaved, auto stream_past) {
@@ -174,9 +174,8 @@ extern "C" int ddp_rotary_table(int rotated, const double *freq, double amplitud
         if (rows == 0) return DDP_OK;
         Frequencies f{};
         for (int i = 0; i < rotated / 2; ++i) f.f[i] = freq[i];
-        const int64_t n = rows * (rotated / 2);
-        if (cdiv(n, 256) > 0x7fffffff) return bad(who, DDP_EINVAL, "the table is too large");
-        hipLaunchKernelGGL(table_kernel, dim3((unsigned)cdiv(n, 256)), dim3(256), 0, static_cast<hipStream_t>(stream), f, amplitude, n, rotated / 2, table);
+        const int64_t n = rows * (rotated / 2), wgs = cdiv(n, 256);
+        hipLaunchKernelGGL(table_kernel, dim3((unsigned)(wgs < most_groups(256) ? wgs : most_groups(256))), dim3(256), 0, static_cast<hipStream_t>(stream), f, amplitude, n, rotated / 2, table);
         return launched(who);
     });
 }
