@@ -285,18 +285,21 @@ __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *part_w, co
     T *out = blockIdx.y ? db : dw;
     if (!out) return;
     const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + col;
-    float s = 0.0f;
-    if (c < cols)
+    for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < cols; c0 += (int64_t)gridDim.x * 32) {
+        const int64_t c = c0 + col;
+        float s = 0.0f;
+        if (c < cols)
 #pragma unroll 8
-        for (int i = r; i < parts; i += 32) s += part[i * cols + c];
-    run[r][col] = s;
-    __syncthreads();
-    if (r == 0 && c < cols) {
-        s = 0.0f;
+            for (int i = r; i < parts; i += 32) s += part[i * cols + c];
+        run[r][col] = s;
+        __syncthreads();
+        if (r == 0 && c < cols) {
+            s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) s += run[i][col];
-        out[c] = (T)s;
+            for (int i = 0; i < 32; ++i) s += run[i][col];
+            out[c] = (T)s;
+        }
+        __syncthreads();  // (the runs may still be read for these columns)
     }
 }
 
@@ -439,9 +442,11 @@ extern "C" int ddp_norm_backward(const ddp_norm *norm, const void *dy, const voi
                             });
                     }
                 });
-            if (columns)
-                hipLaunchKernelGGL((norm_fold_kernel<T>), dim3((unsigned)cdiv(n.cols, 32), dbias ? 2 : 1), dim3(1024), 0, st, a.part_w, a.part_b, parts, n.cols,
-                                   static_cast<T *>(dweight), static_cast<T *>(dbias));
+            if (columns) {
+                const int64_t wgs = cdiv(n.cols, 32);
+                hipLaunchKernelGGL((norm_fold_kernel<T>), dim3((unsigned)(wgs < most_groups(1024) ? wgs : most_groups(1024)), dbias ? 2 : 1), dim3(1024), 0, st, a.part_w,
+                                   a.part_b, parts, n.cols, static_cast<T *>(dweight), static_cast<T *>(dbias));
+            }
             return launched(who);
         });
     });

@@ -34,3 +34,22 @@ def test_a_table_of_more_pairs_than_a_grid_has_threads():
     a = at.double()[:, None] * 500000.0 ** (-torch.arange(128, dtype=torch.float64, device="cuda") * 2 / 256)
     # half a unit of fp32, and the angle's own rounding in 64 bits: angles up to 2^25, two units of them
     assert ((table[at].double() - torch.stack([a.cos(), a.sin()], -1)).abs() <= 2.0 ** -24 + 2.0 ** -26).all()
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_norm_of_rows_of_2_to_the_27(kind):
+    """The weight's gradient has 32 columns a workgroup of 1024 threads."""
+    from paper_2502_11058_amd import operators as O
+    cols = (1 << 27) + 7
+    g = generator(3)
+    x, dy = (torch.empty(2, cols, device="cuda", dtype=torch.bfloat16).normal_(generator=g) for _ in range(2))
+    w = torch.ones(cols, device="cuda", dtype=torch.bfloat16)
+    y, mean, rstd = O.norm_forward(x, w, kind=kind)
+    dx, dw, db = O.norm_backward(dy, x, w, mean, rstd, kind=kind, bias=True)
+    for a in range(0, cols, 1 << 24):
+        at = slice(a, a + (1 << 24))
+        h, d = (x[:, at].float() - (mean[:, None] if kind == "layer" else 0.0)) * rstd[:, None], dy[:, at].float()
+        # from the mean and rstd that the call gave: a few units of fp32, rounded to bf16
+        for got, terms in ((dw[at], d * h), (db[at], d)):
+            assert ((got.float() - terms.sum(0)).abs() <= 8 * EPS * (terms.abs().sum(0) + d.abs().sum(0)) + 2.0 ** -8 * terms.sum(0).abs()).all(), a
+        assert ((y[:, at].float() - h).abs() <= 8 * EPS * (h.abs() + 1) + 2.0 ** -8 * h.abs()).all(), a
