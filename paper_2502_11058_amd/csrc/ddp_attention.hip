@@ -61,7 +61,8 @@ struct AttentionArgs {
     int q_heads, k_heads, dim, batch;
     float scale;
     int causal;
-    int blocks;  // blocks of kRows rows of one head in the grid
+    int blocks;      // blocks of kRows rows of one head in the call
+    unsigned first;  // workgroup of the call that is this launch's first
 };
 
 // One sequence's rows.
@@ -360,8 +361,9 @@ __global__ __launch_bounds__((256 * kParts<T, DP>), (kForwardWaves<T, DP>)) void
     constexpr int PARTS = kParts<T, DP>, OWN = kTile<T>, BN = OWN * PARTS, ROWB = DP * 2, PLANE = BN * ROWB, KS = DP / 16, NS = OWN / 32, DS = DP / 32;
     typedef Tiles<T, DP, BN, 256 * PARTS> Load;
     __shared__ __attribute__((aligned(1024))) char k0_lds[Load::BYTES], v0_lds[Load::BYTES], k1_lds[Load::BYTES], v1_lds[Load::BYTES];
-    const int head = blockIdx.x % a.q_heads, portion = blockIdx.x / a.q_heads % a.portions;
-    const int order = a.blocks - 1 - blockIdx.x / a.q_heads / a.portions;  // the last queries see the most keys: first
+    const unsigned in_call = a.first + blockIdx.x;
+    const int head = in_call % a.q_heads, portion = in_call / a.q_heads % a.portions;
+    const int order = a.blocks - 1 - in_call / a.q_heads / a.portions;  // the last queries see the most keys: first
     Sequence s;
     if (!find_sequence<false>(a, order, s)) return;
     const bool packed = a.cu_q != nullptr;
@@ -532,8 +534,9 @@ __global__ __launch_bounds__((256 * kParts<T, DP>), (kDqWaves<T, DP>)) void atte
     constexpr int PARTS = kParts<T, DP>, OWN = kTile<T>, BN = OWN * PARTS, ROWB = DP * 2, PLANE = BN * ROWB, KS = DP / 16, NS = OWN / 32, DS = DP / 32;
     typedef Tiles<T, DP, BN, 256 * PARTS> Load;
     __shared__ __attribute__((aligned(1024))) char k0_lds[Load::BYTES], v0_lds[Load::BYTES], k1_lds[Load::BYTES], v1_lds[Load::BYTES];
-    const int head = blockIdx.x % a.q_heads, portion = blockIdx.x / a.q_heads % a.portions;
-    const int order = a.blocks - 1 - blockIdx.x / a.q_heads / a.portions;
+    const unsigned in_call = a.first + blockIdx.x;
+    const int head = in_call % a.q_heads, portion = in_call / a.q_heads % a.portions;
+    const int order = a.blocks - 1 - in_call / a.q_heads / a.portions;
     Sequence s;
     if (!find_sequence<false>(a, order, s)) return;
     const bool packed = a.cu_q != nullptr;
@@ -624,9 +627,10 @@ __global__ __launch_bounds__((kDkdvThreads<T, DP>), (kDkdvWaves<T, DP>)) void at
     __shared__ __attribute__((aligned(1024))) char q0_lds[Load::BYTES], d0_lds[Load::BYTES], q1_lds[Load::BYTES], d1_lds[Load::BYTES];
     __shared__ __attribute__((aligned(1024))) char k_lds[WIDE ? kRows * ROWB : 16], v_lds[WIDE ? kRows * ROWB : 16];
     __shared__ __attribute__((aligned(256))) float stat0[2 * 64], stat1[2 * 64];  // the tile's lse2 and delta
-    const int kv_head = blockIdx.x % a.k_heads, portion = blockIdx.x / a.k_heads % a.portions;
+    const unsigned in_call = a.first + blockIdx.x;
+    const int kv_head = in_call % a.k_heads, portion = in_call / a.k_heads % a.portions;
     Sequence s;
-    if (!find_sequence<true>(a, blockIdx.x / a.k_heads / a.portions, s)) return;
+    if (!find_sequence<true>(a, in_call / a.k_heads / a.portions, s)) return;
     const bool packed = a.cu_q != nullptr;
     const int share = a.q_heads / a.k_heads, first_head = kv_head * share;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5;
@@ -937,6 +941,15 @@ struct BackwardLayout {
         bytes = copies + copied;
     }
 };
+// f(workgroups): a call's workgroups in as many launches as grids have room for them.
+template <class F>
+void in_launches(AttentionArgs &a, int heads, int threads, F &&f) {
+    const int64_t all = (int64_t)a.blocks * heads * a.portions, most = most_groups(threads);
+    for (int64_t at = 0; at < all; at += most) {
+        a.first = (unsigned)at;
+        f(dim3((unsigned)(all - at < most ? all - at : most)));
+    }
+}
 template <class T, bool DQ>
 void join_queries(const ddp_attention &at, const AttentionArgs &a, hipStream_t st) {
     const int64_t n = cdiv((at.packed ? 1 : at.batch) * at.q_tokens * at.q_heads * cdiv(at.head_dim, 4), 256);
@@ -979,7 +992,8 @@ extern "C" int ddp_attention_forward(const ddp_attention *attention, const ddp_h
         a.blocks = (int)blocks_of(at, false);
         by_form(at, [&](auto t, auto dp) {
             typedef decltype(t) T;
-            hipLaunchKernelGGL((attention_forward_kernel<T, dp.value>), dim3((unsigned)a.blocks * (unsigned)a.q_heads * (unsigned)a.portions), dim3((256 * kParts<T, dp.value>)), 0, st, a);
+            constexpr int threads = 256 * kParts<T, dp.value>;
+            in_launches(a, a.q_heads, threads, [&](dim3 grid) { hipLaunchKernelGGL((attention_forward_kernel<T, dp.value>), grid, dim3(threads), 0, st, a); });
             if (a.portions > 1) join_queries<Out<T>, false>(at, a, st);
         });
         return launched(who);
@@ -1024,13 +1038,15 @@ extern "C" int ddp_attention_backward(const ddp_attention *attention, const ddp_
             if (at.q_tokens > 0) {  // (first: it leaves lse and do . o for dk and dv)
                 a.blocks = (int)blocks_of(at, false);
                 a.portions = query_portions(at);
-                hipLaunchKernelGGL((attention_dq_kernel<T, dp.value>), dim3((unsigned)a.blocks * (unsigned)a.q_heads * (unsigned)a.portions), dim3((256 * kParts<T, dp.value>)), 0, st, a);
+                constexpr int threads = 256 * kParts<T, dp.value>;
+                in_launches(a, a.q_heads, threads, [&](dim3 grid) { hipLaunchKernelGGL((attention_dq_kernel<T, dp.value>), grid, dim3(threads), 0, st, a); });
                 if (a.portions > 1) join_queries<Out<T>, true>(at, a, st);
             }
             if (at.k_tokens > 0) {
                 a.blocks = (int)blocks_of(at, true);
                 a.portions = key_portions(at);
-                hipLaunchKernelGGL((attention_dkdv_kernel<T, dp.value>), dim3((unsigned)(a.blocks * a.k_heads * a.portions)), dim3((kDkdvThreads<T, dp.value>)), 0, st, a);
+                constexpr int threads = kDkdvThreads<T, dp.value>;
+                in_launches(a, a.k_heads, threads, [&](dim3 grid) { hipLaunchKernelGGL((attention_dkdv_kernel<T, dp.value>), grid, dim3(threads), 0, st, a); });
                 if (a.portions > 1) {
                     const int64_t n = cdiv((at.packed ? 1 : at.batch) * at.k_tokens * at.k_heads * cdiv(at.head_dim, 4), 256);
                     hipLaunchKernelGGL((attention_join_kernel<Out<T>>), dim3((unsigned)(n < (1 << 20) ? n : 1 << 20), 2), dim3(256), 0, st, a);

@@ -53,3 +53,26 @@ def test_norm_of_rows_of_2_to_the_27(kind):
         for got, terms in ((dw[at], d * h), (db[at], d)):
             assert ((got.float() - terms.sum(0)).abs() <= 8 * EPS * (terms.abs().sum(0) + d.abs().sum(0)) + 2.0 ** -8 * terms.sum(0).abs()).all(), a
         assert ((y[:, at].float() - h).abs() <= 8 * EPS * (h.abs() + 1) + 2.0 ** -8 * h.abs()).all(), a
+
+
+@pytest.mark.parametrize("dtype,batch,dim", [(torch.float32, (1 << 20) + 1, 8), (torch.bfloat16, (1 << 20) + 1, 72), (torch.bfloat16, (1 << 21) + 1, 8)])
+def test_attention_of_more_heads_than_a_grid_has_workgroups(dtype, batch, dim):
+    """8 heads of so many sequences with one query and key each, a workgroup of 256 or 512 threads a head: o is v, dv is do, and nothing is left
+    for dq and dk."""
+    from paper_2502_11058_amd import operators as O
+    g = generator(batch + dim)
+    q, k, v, do = (torch.empty(batch, 1, 8, dim, device="cuda", dtype=dtype).normal_(generator=g) for _ in range(4))
+    o, lse = O.attention_forward(q, k, v)
+    dq, dk, dv = O.attention_backward(do, q, k, v, o, lse)
+    fine = 2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -18
+    for a in range(0, batch, 1 << 18):
+        at = slice(a, a + (1 << 18))
+        x, y, u, w = (t[at, 0].double() for t in (q, k, v, do))
+        z, terms = (x * y).sum(-1) * dim ** -0.5, (x * y).abs().sum(-1) * dim ** -0.5
+        # the score's products and sum in fp32, and the logarithm's base changed both ways; that much of p, which is 1, is off
+        assert ((lse[at, :, 0].double() - z).abs() <= 64 * EPS * (terms + 1)).all(), a
+        off = (fine + 64 * EPS * (terms + 1))[..., None]
+        assert ((o[at, 0].double() - u).abs() <= off * u.abs()).all() and ((dv[at, 0].double() - w).abs() <= off * w.abs()).all(), a
+        # do . v and do . o differ by what o was rounded and by fp32
+        off = 2 * off * (w * u).abs().sum(-1, keepdim=True) * dim ** -0.5
+        assert (dq[at, 0].double().abs() <= off * y.abs()).all() and (dk[at, 0].double().abs() <= off * x.abs()).all(), a
