@@ -126,7 +126,8 @@ int ddp_attention_backward(const ddp_attention *attention, const ddp_heads *d_o,
  *   x, dx            [tokens, hidden] of dtype, x_stride and dx_stride between rows
  *   weight, dweight  [vocab, hidden] of dtype, w_stride and dw_stride between rows
  *   targets          int64 [tokens];  loss, lse, dloss  fp32 [tokens]
- *   dx or dweight may be NULL.  The workspace calls look at x and weight's addresses only, not at what is there: rows whose start, stride or
+ *   dx or dweight may be NULL.  Any two of tokens, vocab and hidden are less than 2^23 tiles of 256 x 256: tokens * vocab up to 2^39.
+ *   The workspace calls look at x and weight's addresses only, not at what is there: rows whose start, stride or
  *   hidden are no multiples of 16 and 128 bytes, and fp32 ones of more than 64 tokens, are copied into padded ones in the workspace.
  * z is formed piece by piece of the vocabulary, in the backward call again; dz is rounded to dtype as an operand of the second
  * products, whose sums are fp32. */

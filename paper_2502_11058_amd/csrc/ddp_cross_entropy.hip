@@ -779,13 +779,16 @@ struct Layout {  // of a call's workspace; offsets in bytes
 int check_head(const char *who, const ddp_head *h) {
     if (!h) return bad(who, DDP_EINVAL, "the shape is NULL");
     if (!typed(h->dtype)) return bad(who, DDP_EINVAL, "dtype must be DDP_F32 or DDP_BF16");
-    if (h->tokens < 0 || h->tokens > (1 << 30)) return bad(who, DDP_EINVAL, "tokens must be in [0, 2^30]");
-    if (h->vocab < 1 || h->vocab > (1 << 30)) return bad(who, DDP_EINVAL, "vocab must be in [1, 2^30]");
+    // (16 tokens, or 64 words, are a workgroup of 256 threads)
+    if (h->tokens < 0 || h->tokens > 16 * most_groups(256)) return bad(who, DDP_EINVAL, "tokens must be in [0, 2^28 - 16]");
+    if (h->vocab < 1 || h->vocab > 64 * most_groups(256)) return bad(who, DDP_EINVAL, "vocab must be in [1, 2^30 - 64]");
     if (h->hidden < 1 || h->hidden > (1 << 20)) return bad(who, DDP_EINVAL, "hidden must be in [1, 2^20]");
     if ((h->tokens > 1 && h->x_stride < h->hidden) || (h->vocab > 1 && h->w_stride < h->hidden)) return bad(who, DDP_EINVAL, "rows overlap: a stride is smaller than hidden");
     if (reach(h->tokens, h->x_stride) < 0 || reach(h->vocab, h->w_stride) < 0) return bad(who, DDP_EINVAL, "a stride is too large");
-    if (cdiv(h->tokens, 64) * cdiv(h->vocab, 128) > 0x7fffffff || cdiv(h->hidden, 128) * cdiv(h->vocab, 64) > 0x7fffffff)
-        return bad(who, DDP_EINVAL, "too many tiles");
+    // (the large tiles: products of few of them, which take small ones, are far from it)
+    const int64_t tokens = cdiv(h->tokens, 256), words = cdiv(h->vocab, 256), columns = cdiv(h->hidden, 256), most = most_groups(512);
+    if (tokens * words > most || columns * words > most || columns * tokens > most)
+        return bad(who, DDP_EINVAL, "more than 2^23 tiles of 256 x 256: split the tokens over several calls");
     return DDP_OK;
 }
 
