@@ -77,7 +77,7 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[torch.Tensor, int, int]:
     if not (t.dim() >= 1):
         raise ValueError(f"{name} needs a dimension")
     r = t if t.dim() == 2 else t.reshape(-1, t.shape[-1])
-    if r.shape[1] > 1 and (r.stride(1) != 1 or (r.shape[0] > 1 and r.stride(0) < r.shape[1])):
+    if (r.shape[1] > 1 and r.stride(1) != 1) or (r.shape[0] > 1 and r.stride(0) < r.shape[1]):
         r = r.contiguous()
     return r, r.shape[0], r.stride(0)
 
