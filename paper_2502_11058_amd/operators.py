@@ -257,7 +257,7 @@ def _attention_shape(q, k, v, causal, scale, cu_q, cu_k) -> Tuple[B.ddp_attentio
     else:
         batch, q_tokens, heads, dim = of_q
         k_tokens, k_heads, of_lse = of_k[1], of_k[2], (batch, heads, q_tokens)
-    return B.ddp_attention(dtype, bool(causal), heads, k_heads, dim, batch, q_tokens, k_tokens, dim ** -0.5 if scale is None else scale, packed), packed, of_q, of_lse
+    return B.ddp_attention(dtype, bool(causal), heads, k_heads, dim, batch, q_tokens, k_tokens, max(dim, 1) ** -0.5 if scale is None else scale, packed), packed, of_q, of_lse
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = True, scale: Optional[float] = None,

@@ -24,3 +24,13 @@ def test_one_column_expanded():
     assert torch.equal(y, want[0]) and torch.equal(rstd, want[2])
     for a, b in zip(O.norm_backward(dy[:1].expand(5, 1), x, w, None, rstd, kind="rms"), O.norm_backward(dy[:1].repeat(5, 1), x.contiguous(), w, None, rstd, kind="rms")):
         assert a is b is None or torch.equal(a, b)
+
+
+def test_heads_without_channels(monkeypatch):
+    """Refused by the library, as other sizes that it does not take are."""
+    B.lib()
+    monkeypatch.setattr(O, "_typed", lambda first: 0)
+    q = torch.zeros(1, 3, 2, 0)
+    with pytest.raises(B.DdpError) as e:
+        O.attention_forward(q, q, q)
+    assert e.value.code == 1 and "head_dim" in str(e.value)
