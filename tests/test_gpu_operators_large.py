@@ -76,3 +76,105 @@ def test_attention_of_more_heads_than_a_grid_has_workgroups(dtype, batch, dim):
         # do . v and do . o differ by what o was rounded and by fp32
         off = 2 * off * (w * u).abs().sum(-1, keepdim=True) * dim ** -0.5
         assert (dq[at, 0].double().abs() <= off * y.abs()).all() and (dk[at, 0].double().abs() <= off * x.abs()).all(), a
+
+
+# ---- offsets beyond 2^31 elements ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_of_more_than_2_to_the_31_elements(dtype):
+    from paper_2502_11058_amd import operators as O
+    rows, cols = (1 << 20) + 5, 2056
+    g = generator(5)
+    x, dy = (torch.empty(rows, cols, device="cuda", dtype=dtype).normal_(generator=g) for _ in range(2))
+    w, b = (torch.empty(cols, device="cuda", dtype=dtype).normal_(generator=g) for _ in range(2))
+    y, mean, rstd = O.norm_forward(x, w, b)
+    dx, dw, db = O.norm_backward(dy, x, w, mean, rstd, bias=True)
+    sums = torch.zeros(2, cols, device="cuda", dtype=torch.float64)
+    squares = torch.zeros_like(sums)
+    fine = 2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -23
+    for a in range(0, rows, 1 << 16):
+        at = slice(a, a + (1 << 16))
+        u, d = x[at].double(), dy[at].double()
+        m = u.mean(1, keepdim=True)
+        r = 1 / torch.sqrt(((u - m) ** 2).mean(1, keepdim=True) + 1e-5)
+        h = (u - m) * r
+        # fp32 knows the mean, h and what they are multiplied with to a few units
+        assert ((y[at].double() - (h * w.double() + b.double())).abs() <= 16 * EPS * ((h.abs() + 1) * w.double().abs() + b.double().abs()) + fine * y[at].double().abs()).all(), a
+        e = d * w.double()
+        want = r * (e - e.mean(1, keepdim=True) - h * (e * h).mean(1, keepdim=True))
+        assert ((dx[at].double() - want).abs() <= 16 * EPS * r * (e.abs() + e.abs().mean(1, keepdim=True) * (1 + h.abs()) * 2) + fine * want.abs()).all(), a
+        for i, t in enumerate((d * h, d)):
+            sums[i] += t.sum(0)
+            squares[i] += (t * t).sum(0)
+    # a thousand partial sums of a thousand terms each, in fp32: each off by some units of its root-mean-square size, at random
+    for got, want, sq in ((dw, sums[0], squares[0]), (db, sums[1], squares[1])):
+        assert ((got.double() - want).abs() <= 64 * EPS * sq.sqrt() + fine * want.abs()).all()
+
+
+def test_rotary_of_more_than_2_to_the_31_elements():
+    from paper_2502_11058_amd import operators as O
+    n, heads, dim = (1 << 20) + 5, 16, 136
+    g = generator(6)
+    q = torch.empty(n, heads, dim, device="cuda", dtype=torch.bfloat16).normal_(generator=g)
+    p = torch.randint(0, 512, (n,), generator=g, device="cuda")
+    table = O.rotary_table(512, 128)
+    got, _ = O.rotary_forward(q, None, table, p, layout="interleaved")
+    for a in range(0, n, 1 << 17):
+        x, y, t = q[a:a + (1 << 17)].float(), got[a:a + (1 << 17)].float(), table[p[a:a + (1 << 17)]][:, None]
+        c, s, u, v = t[..., 0], t[..., 1], x[..., 0:128:2], x[..., 1:128:2]
+        room = 4 * EPS * (u.abs() + v.abs())
+        for part, want in ((y[..., 0:128:2], u * c - v * s), (y[..., 1:128:2], u * s + v * c)):
+            assert ((part - want).abs() <= room + 2.0 ** -8 * want.abs()).all(), a
+        assert torch.equal(x[..., 128:], y[..., 128:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_to_a_cache_of_more_than_2_to_the_31_elements(dtype):
+    """The last five tokens of a million, 17 heads of 124 channels."""
+    from test_gpu_operators_attention import _check
+    g = generator(7)
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    q, do = (torch.empty(1, 5, 17, 124, device="cuda", dtype=t).normal_(generator=g) for _ in range(2))
+    k, v = (torch.empty(1, (1 << 20) + 77, 17, 124, device="cuda", dtype=t).normal_(generator=g) for _ in range(2))
+    _check(q, k, v, do)
+
+
+@pytest.mark.parametrize("dtype,tokens", [(torch.float32, 40), (torch.float32, 70), (torch.bfloat16, 70)])
+def test_a_head_of_more_than_2_to_the_31_elements(dtype, tokens):
+    from operator_bounds import TINY, near, over
+    from paper_2502_11058_amd import operators as O
+    vocab, hidden, step = (1 << 19) + 77, 4160, 1 << 15
+    g = generator(tokens)
+    x = torch.empty(tokens, hidden, device="cuda", dtype=dtype).normal_(generator=g)
+    w = torch.empty(vocab, hidden, device="cuda", dtype=dtype).normal_(0, 1.5 / hidden ** 0.5, generator=g)
+    t = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
+    t[0], t[1], grad = vocab - 1, -100, torch.rand(tokens, generator=g, device="cuda") + 0.5
+    loss, lse = O.linear_cross_entropy_forward(x, w, t)
+    dx, dw = O.linear_cross_entropy_backward(grad, x, w, t, lse)
+    # as in the tests of small sizes, the weight taken in pieces
+    u, xd = (2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -24), x.double()
+    pieces = [slice(a, a + step) for a in range(0, vocab, step)]
+    z, terms = (torch.cat([f(xd, w[p].double()) for p in pieces], 1) for f in (lambda a, b: a @ b.t(), lambda a, b: a.abs() @ b.t().abs()))
+    valid, gd = t >= 0, torch.where(t >= 0, grad.double(), 0.0)
+    want_lse, at = torch.logsumexp(z, 1), t.clamp(min=0)[:, None]
+    p = torch.exp(z - want_lse[:, None])
+    off_z = over(hidden) * terms + 4 * EPS * z.abs()
+    off_lse = 2 * (p * off_z).sum(1) + 4 * EPS * want_lse.abs() + over(vocab)
+    near(lse, want_lse, off_lse, "lse")
+    near(loss, torch.where(valid, want_lse - z.gather(1, at)[:, 0], 0.0), off_lse + off_z.gather(1, at)[:, 0] + 4 * EPS * z.gather(1, at)[:, 0].abs(), "loss")
+    hot = torch.zeros_like(p).scatter_(1, at, 1.0)
+    dz = (p - hot) * gd[:, None]
+    off = (p * (off_z + off_lse[:, None]) + (u + 8 * EPS) * (p - hot).abs() + 4 * EPS * p + TINY) * gd[:, None]
+    want, room = (torch.zeros(tokens, hidden, device="cuda", dtype=torch.float64) for _ in range(2))
+    for i in pieces:
+        wd = w[i].double()
+        want += dz[:, i] @ wd
+        room += (off[:, i] + over(vocab) * dz[:, i].abs()) @ wd.abs()
+        near(dw[i], dz[:, i].t() @ xd, off[:, i].t() @ xd.abs() + over(tokens) * (dz[:, i].abs().t() @ xd.abs()), f"dweight from {i.start}")
+    near(dx, want, room, "dx")
+
+
+def test_several_pieces_of_the_vocabulary_in_fp32():
+    """dz is three planes there, whose distance is another in the last piece, which is shorter."""
+    from test_gpu_operators_cross_entropy import _check, _inputs
+    _check(*_inputs(23, "f32", 9000, 20011, 64))
