@@ -6,7 +6,8 @@ without logits in memory.  Projections are plain matrix products (torch).
 
 Tokens are synthetic: a random walk over the vocabulary that the model can learn.  The peers' buffers stand for N - 1 workers that
 have drifted from this one (Gaussian, as in the benchmark).  Llama-shaped workloads: root-mean-square norm, rotary positions, shared key heads,
-gated feed-forward block.  GPT-2-shaped: layer norm, learned positions, the embedding as the head.
+gated feed-forward block.  GPT-2-shaped: layer norm, learned positions, the embedding as the head: one parameter, whose gradient autograd
+adds up from both uses before its hook fires, behind the last kernel that reads it.
 """
 from __future__ import annotations
 
