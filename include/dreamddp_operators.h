@@ -97,8 +97,8 @@ int ddp_rotary(const ddp_rotary_shape *shape, const void *q, const void *k, cons
  * may be parts of one projection's output); others, and fp32 ones as three bf16 planes whose products are as exact as fp32's, are
  * copied into the workspace.  The workspace calls look at the tensors' addresses and strides only; NULL: as if copied.
  * Where heads and blocks of queries (keys) are few, parts of a sum over the keys (queries) lie in the workspace as well, in fp32.
- * A key that a query does not see has p = 0, which multiplies its value: a value that is not finite may make queries of the sequence NaN that do not
- * see it, as a masked product would.
+ * A pair of a query and a key that it does not see has p = ds = 0, which multiply the pair's rows in the second products: values that are not finite, and
+ * in the backward call such keys, queries and d_o, may make rows of the sequence NaN that they are masked from, as a masked product would.
  * In bf16 the probabilities and ds are rounded to bf16 as operands of the second products, whose sums are fp32. */
 typedef struct {
     void *data;

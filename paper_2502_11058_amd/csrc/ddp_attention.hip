@@ -12,11 +12,13 @@
 // do not depend on any order, and where nothing is split no fp32 copy of a gradient is needed.
 //
 // What bounds it, 8192 causal tokens, 32 heads of 128 over 8, bf16: the matrix cores and the exponentials' vector instructions by turns, at the
-// 1.6 GHz that their power leaves (forward: matrix cores busy 57 % of the time, vector units 59 %, .57 ms, .97 Pflop/s; dq 60 and 56 %, 1.08 ms;
-// dk and dv 53 and 40 %, 1.28 ms).  Tiles of 64 keys (32 in fp32, three planes) are what two pairs of buffers, the next pair on its way while one
+// 1.6 GHz that their power leaves (forward: matrix cores busy 57 % of the time, vector units 59 %, .57 to .64 ms, .86 to .97 Pflop/s; dq 60 and
+// 56 %, 1.06 ms; dk and dv 53 and 40 %, 1.27 ms).  Tiles of 64 keys (32 in fp32, three planes) are what two pairs of buffers, the next pair on its way while one
 // is worked on, leave room for beside a second workgroup.
 //
-// In bf16, dO . O of the rounded O is off by as much as a rounding of ds, in every ds of a row alike.  The rows' ds have to sum to zero; what
+// In bf16 the second products' operands, p and ds, are rounded to bf16, which is what the matrix instruction for bf16 takes: planes of them as
+// for fp32 would be three times the products.  Results are up to 1.4 times as far from 64 bits for it as their own rounding makes them.
+// dO . O of the rounded O is off by as much as a rounding of ds, in every ds of a row alike.  The rows' ds have to sum to zero; what
 // they sum to in the dq kernel is that error, and the dk and dv kernel, which runs behind it, has dO . O without.  dq's own ds are
 // multiplied with their rounding's remainder too: an eighth product.  Errors of dq and dk against 64 bits, 6001 tokens in 11 documents:
 // 2.6e-3 without both, 2.0e-3 and 2.3e-3 with them; 1.7e-3 is the result's own rounding.

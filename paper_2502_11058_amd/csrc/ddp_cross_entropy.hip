@@ -6,8 +6,11 @@
 //   forward    a tile's logits stay in registers, and only their maximum and sum of exponentials per token leave it
 //   backward   a tile becomes dz in dtype, for a piece of the vocabulary at a time, and two products go over the piece
 //
-// Measured, 8192 tokens, 128256 words of 4096 in bf16: logits 6.9 to 7.2 ms, and for each of eight pieces dz .90, dx .88, dweight .89 ms: 1.19 to 1.25
-// Pflop/s.  fp32, 2048 tokens, 50257 words of 768, six bf16 products each: .90, 1.03, .84 and 1.0 ms, 1.0 to 1.15 Pflop/s of them.
+// Measured, 8192 tokens, 128256 words of 4096 in bf16: logits 6.8 to 7.2 ms, and for each of eight pieces dz .89, dx .87, dweight .88 ms: 1.19 to 1.25
+// Pflop/s.  fp32, 2048 tokens, 50257 words of 768, six bf16 products each: .89, .99, .80 and 1.0 ms, 1.0 to 1.15 Pflop/s of them.
+//
+// Registers of the large tiles: the logits kernel keeps 210 scalar ones in lanes of vector registers, dx's product 12 vector ones in scratch memory (52
+// bytes a lane), both outside the loop of the products.
 #include "ddp_operators.h"
 
 namespace ddp {
@@ -505,8 +508,8 @@ __global__ __launch_bounds__(256) void split_dlogits_kernel(const LogitArgs a, c
 
 // ---- fp32 and few tokens -------------------------------------------------------------------------------------------
 // Up to 64 tokens a product of fp32 takes less time on the fp32 matrix instruction (64 flop a cycle and SIMD) than planes of the weight
-// take to write and read (a pass of 16 tokens, 6787 words of 2590: 280 us with planes, 132 so; 53, 15401 of 3002: 545 and 430; 64, 1302 of 123: 67 and
-// 66), so these read the tensors as they lie, each operand straight into registers: four elements of a row a lane, whose places in k
+// take to write and read (a pass of 16 tokens, 6787 words of 2590: 280 us with planes, 127 so; 53, 15401 of 3002: 545 and 425; 64, 1302 of 123: 67 and
+// 65), so these read the tensors as they lie, each operand straight into registers: four elements of a row a lane, whose places in k
 // (or columns) are spread over four instructions; the sum over k has no order to keep.  Lane l of an operand has row (column) l % 32 and k l / 32.
 constexpr int kFew = 64;
 

@@ -27,7 +27,7 @@ class BackwardOverlap:
     same backward pass reads them again (every kernel of the layer's own backward is already queued ahead of the
     event); a model that recomputes activations of that layer afterwards must not be driven this way.  Weights used in
     several places are one parameter, whose gradient is complete, and whose call is made, when the last of its uses has
-    been gone through backwards: that is safe too (a head that is the embedding, as in pretrain.py).  Two registered tensors must not share memory.
+    been gone through backwards: that is safe too (a head that is the embedding, as in pretrain.py), unless one of the uses is of a detached copy.  Two registered tensors must not share memory.
     """
 
     def __init__(self, rep: DeviceReplica, side_stream: Optional[torch.cuda.Stream] = None, side_cus: int = 0):
